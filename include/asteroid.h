@@ -248,7 +248,8 @@ int asteroid_ckpt8_act_backward(int act, const void* ckpt, const void* dy, size_
 /* Parameter gradients of a linear layer from the checkpoint of its input x [rows][c_in] and the gradient dy [rows][c_out] of its output:
  * dw[o][i] = sum over rows of dy[r][o] * (x as kept)[r][i], db[o] = sum over rows of dy[r][o] (db may be NULL), float32 sums, added to
  * what dw and db hold if `accumulate`, else written.  rows = 0 gives zeros.  The order of the sums depends on the sizes, the type and
- * the device only: the same inputs give the same bits.  Should a wait inside the kernel run out, the gradients are NaN.  workspace: 16-byte aligned DEVICE memory of at least
+ * the device only: the same inputs give the same bits.  Should a wait inside the kernel run out, the tiles of dw, with their entries of db,
+ * that it concerns are NaN, all of them.  workspace: 16-byte aligned DEVICE memory of at least
  * asteroid_ckpt8_linear_wgrad_workspace bytes as asked for on this device (may be 0, then workspace may be NULL), not shared by calls that may
  * overlap.
  * c_in, c_out <= 65536. */
@@ -334,6 +335,12 @@ int asteroid_plan(const ast_plan_problem* problem, ast_plan_result* result);
  * the kernel returned (the expected outcome), AST_OK if the wait reported success, AST_ERR_CUDA on a runtime
  * error.  Synchronises the device; the context stays usable. */
 int asteroid_selftest_bounded_wait(void);
+/* The same for asteroid_ckpt8_linear_wgrad, whose call has no status to report by: arguments as there, but rows >= 1 and dy rows that start at 16-byte (float32: 8-byte)
+ * boundaries, with c_out even for float32.  The waits are of some milliseconds, and the pair of multiprocessors that takes the first tile stops
+ * after `silent_after` >= 0 of its steps of 64 rows.  AST_ERR_TIMEOUT (expected) when waits ran out: dw and db are then NaN wherever that pair had a part from there on, and
+ * as ever everywhere else; AST_OK when it had no further step.  Synchronises the device. */
+int asteroid_selftest_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db,
+                                         int accumulate, void* workspace, size_t workspace_bytes, int silent_after);
 
 /* Count of kernel launches this library has enqueued in the calling process. */
 uint64_t asteroid_launch_count(void);

@@ -19,7 +19,7 @@ EXPORTS = ["asteroid_stage_create", "asteroid_stage_create_ckpt8", "asteroid_sta
            "asteroid_ckpt8_bytes", "asteroid_ckpt8_pack", "asteroid_ckpt8_unpack", "asteroid_ckpt8_act_forward", "asteroid_ckpt8_act_backward",
            "asteroid_ckpt8_linear_wgrad_workspace", "asteroid_ckpt8_linear_wgrad", "asteroid_embedding_forward", "asteroid_embedding_workspace",
            "asteroid_embedding_backward", "asteroid_trace_start", "asteroid_trace_stop",
-           "asteroid_selftest_bounded_wait", "asteroid_plan", "asteroid_launch_count", "asteroid_last_error"]
+           "asteroid_selftest_bounded_wait", "asteroid_selftest_ckpt8_linear_wgrad", "asteroid_plan", "asteroid_launch_count", "asteroid_last_error"]
 
 
 class ast_layer(C.Structure):
@@ -115,6 +115,7 @@ def lib():
         L.asteroid_trace_start.argtypes = []
         L.asteroid_trace_stop.argtypes = [C.POINTER(ast_kernel_stat), i, C.POINTER(i)]
         L.asteroid_selftest_bounded_wait.argtypes = []
+        L.asteroid_selftest_ckpt8_linear_wgrad.argtypes = [vp, vp, sz, sz, i, i, i, vp, vp, i, vp, sz, i]
         L.asteroid_plan.argtypes = [C.POINTER(ast_plan_problem), C.POINTER(ast_plan_result)]
         L.asteroid_launch_count.argtypes = []
         L.asteroid_launch_count.restype = C.c_uint64
@@ -290,6 +291,12 @@ def asteroid_trace_stop():
 def asteroid_selftest_bounded_wait():
     """Return code of the bounded-wait self-test (AST_ERR_TIMEOUT is the expected outcome); does not raise."""
     return lib().asteroid_selftest_bounded_wait()
+
+
+def asteroid_selftest_ckpt8_linear_wgrad(ckpt_ptr, dy_ptr, lddy, rows, c_in, c_out, dtype, dw_ptr, db_ptr, accumulate, workspace_ptr, workspace_bytes, silent_after):
+    """Return code of the self-test (AST_ERR_TIMEOUT where a wait was made to run out); does not raise."""
+    return lib().asteroid_selftest_ckpt8_linear_wgrad(ckpt_ptr, dy_ptr, lddy, rows, c_in, c_out, dtype, dw_ptr, db_ptr, accumulate, workspace_ptr, workspace_bytes,
+                                                      silent_after)
 
 
 def asteroid_plan(prob):

@@ -443,8 +443,9 @@ size_t asteroid_ckpt8_linear_wgrad_workspace(size_t rows, int c_in, int c_out, i
     return ckpt8_wgrad_scratch(dtype, rows, c_in, c_out) * sizeof(float);
 }
 
-int asteroid_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db,
-                                int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+// checks and launches of both calls
+static int linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db, int accumulate,
+                        void* workspace, size_t workspace_bytes, int* err, int silent_after, cudaStream_t st) {
     int rc = bad_widths(rows, c_in, c_out, dtype);
     if (rc || (rc = bad_matrix("lddy out of range", dy, lddy, rows, c_out, dtype)) || (rc = bad_ckpt(ckpt, rows))) return rc;
     if (!dw) return report_error(AST_ERR_ARG, "null argument");
@@ -452,9 +453,31 @@ int asteroid_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, s
     const size_t need = ckpt8_wgrad_scratch(dtype, rows, c_in, c_out) * sizeof(float);
     if (need && (!workspace || workspace_bytes < need)) return report_error(AST_ERR_ARG, "the workspace is too small");
     if (need && reinterpret_cast<uintptr_t>(workspace) % 16) return report_error(AST_ERR_ARG, "a workspace must start at a 16-byte boundary");
-    ckpt8_wgrad(dtype, ckpt, exps_of(ckpt, rows, c_in), dy, lddy, rows, c_in, c_out, dw, db, accumulate != 0, static_cast<float*>(workspace), nullptr,
-                (cudaStream_t)stream);
+    ckpt8_wgrad(dtype, ckpt, exps_of(ckpt, rows, c_in), dy, lddy, rows, c_in, c_out, dw, db, accumulate != 0, static_cast<float*>(workspace), err, st, silent_after);
     return launched();
+}
+
+int asteroid_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db,
+                                int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+    return linear_wgrad(ckpt, dy, lddy, rows, c_in, c_out, dtype, dw, db, accumulate, workspace, workspace_bytes, nullptr, -1, (cudaStream_t)stream);
+}
+
+int asteroid_selftest_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db,
+                                         int accumulate, void* workspace, size_t workspace_bytes, int silent_after) {
+    const size_t unit = dtype == AST_F32 ? 2 : 8;
+    if (silent_after < 0 || rows < 1 || lddy % unit || reinterpret_cast<uintptr_t>(dy) % (unit == 2 ? 8 : 16) || (dtype == AST_F32 && c_out % 2))
+        return report_error(AST_ERR_ARG, "the self-test takes rows of dy at 16-byte (float32: 8-byte) boundaries, and a number of steps");
+    int *err = nullptr, h = 0;
+    cudaError_t e = cudaMalloc((void**)&err, sizeof(int));
+    if (e == cudaSuccess) e = cudaMemset(err, 0, sizeof(int));
+    int rc = AST_OK;
+    if (e == cudaSuccess) rc = linear_wgrad(ckpt, dy, lddy, rows, c_in, c_out, dtype, dw, db, accumulate, workspace, workspace_bytes, err, silent_after, 0);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(&h, err, sizeof h, cudaMemcpyDeviceToHost);
+    cudaFree(err);
+    if (rc) return rc;
+    if (e != cudaSuccess) return report_error(AST_ERR_CUDA, cudaGetErrorString(e));
+    return h ? report_error(AST_ERR_TIMEOUT, "a bounded device-side wait expired (self-test: expected)") : AST_OK;
 }
 
 }  // extern "C"

@@ -72,6 +72,7 @@ struct WArgs {
     float *dw, *db, *part;         // part [parts][rest][2] blocks of part_floats(nt)
     int add;
     int* err;                      // device error word, may be null
+    int silent_after;              // self-test: steps after which the first pair's leading CTA announces nothing more
 };
 __host__ __device__ inline size_t part_floats(int nt) { return (size_t)HALF_M * nt + HALF_M; }     // a CTA's accumulators, then its bias gradient
 
@@ -115,8 +116,10 @@ __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
 __device__ __forceinline__ void announce_at(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// bounded; gives up as soon as another role of the CTA has
-__device__ __forceinline__ bool wait_for(uint32_t mbar, uint32_t parity, volatile int* gave_up) { return mbar_wait_abortable(mbar, parity, gave_up); }
+// bounded (PROBE: some milliseconds); gives up as soon as another role of the CTA has
+template <bool PROBE> __device__ __forceinline__ bool wait_for(uint32_t mbar, uint32_t parity, volatile int* gave_up) {
+    return mbar_wait_abortable(mbar, parity, gave_up, PROBE ? 1u << 14 : WAIT_LIMIT);
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
                  "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
@@ -137,9 +140,9 @@ __device__ __forceinline__ uint32_t test_wait(uint32_t mbar, uint32_t parity) {
     return ok;
 }
 // ... by a whole warp, with one answer
-__device__ __forceinline__ bool warp_wait_for(uint32_t mbar, uint32_t parity, volatile int* gave_up) {
+template <bool PROBE> __device__ __forceinline__ bool warp_wait_for(uint32_t mbar, uint32_t parity, volatile int* gave_up) {
     if (__all_sync(0xffffffffu, mbar_try_wait(mbar, parity))) return true;
-    return __all_sync(0xffffffffu, wait_for(mbar, parity, gave_up));
+    return __all_sync(0xffffffffu, wait_for<PROBE>(mbar, parity, gave_up));
 }
 __device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap* m, int c0, int c1, uint32_t mbar) {
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
@@ -224,7 +227,8 @@ __device__ __forceinline__ void cut3(float f, uint32_t* t) {
     t[2] = __float_as_uint(r - __uint_as_float(t[1])) & 0xffff0000u;
 }
 
-template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const WArgs a) {
+// PROBE: the self-test's, with short waits, which are made to run out
+template <int MODE, bool PROBE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const WArgs a) {
     constexpr int S = Form<MODE>::S, STAGE = Form<MODE>::STAGE, TERMS = Form<MODE>::TERMS, SPAN = Form<MODE>::SPAN;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t bars[3 * S + 2];
@@ -282,7 +286,7 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
                 tile_at(a, w.tile, &m, &n);
                 const int x = m * TILE_M + (int)rank * HALF_M, y1 = w.k1 * ROWS;
                 for (int y = w.k0 * ROWS; y < y1; y += ROWS) {
-                    if (!(ok = wait_for(empty(s), parity, gave_up))) break;
+                    if (!(ok = wait_for<PROBE>(empty(s), parity, gave_up))) break;
                     const uint32_t dst = smem_u32(base) + s * STAGE;
                     if (rank == 0) mbar_expect_tx(full(s), 2 * A_BYTES);
                     pair_load_2d(dst, &tm_dy, x, y, to + 8u * s);
@@ -313,13 +317,13 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
                 uint32_t more = 0;
                 for (int k = w.k0, left = 0; k < w.k1; ++k, --left) {
                     if (!left) {                         // a span begins
-                        if (done && !(ok = warp_wait_for(acc_read, (uint32_t)((done - 1) & 1), gave_up))) break;
+                        if (done && !(ok = warp_wait_for<PROBE>(acc_read, (uint32_t)((done - 1) & 1), gave_up))) break;
                         left = SPAN;
                         more = 0;
                         ++done;
                     }
                     // a look at a barrier takes 200 cycles while the converting warps use shared memory: the next step's is asked for before this one's work is issued
-                    if (!__all_sync(0xffffffffu, ready) && !(ok = warp_wait_for(full(s), parity, gave_up))) break;
+                    if (!__all_sync(0xffffffffu, ready) && !(ok = warp_wait_for<PROBE>(full(s), parity, gave_up))) break;
                     fence_after_sync();
                     const int ns = s + 1 == S ? 0 : s + 1;
                     const uint32_t np = ns ? parity : parity ^ 1u;
@@ -337,6 +341,7 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
                     parity = np;
                 }
             }
+            for (int i = 0; !ok && i < 10000; ++i) __nanosleep(1000);            // ... and instructions in flight end
         }
     } else if (warp == 2) {
         // What the CTA's converting warps have written, made visible to the tensor core and announced to the leading CTA.  A warp of its own does that: the
@@ -346,10 +351,12 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
             int s = 0;
             uint32_t parity = 0;
             bool ok = true;
+            int announced = 0;
             for (int u = pair; u < n_units && ok; u += pairs) {
                 const Unit w = unit_of(a, u);
                 for (int k = w.k0; k < w.k1; ++k) {
-                    if (!(ok = wait_for(written(s), parity, gave_up))) break;
+                    if (!(ok = wait_for<PROBE>(written(s), parity, gave_up))) break;
+                    if (PROBE && !(ok = blockIdx.x || announced++ < a.silent_after)) break;
                     fence_async_smem();
                     announce_at(to + 8u * s);
                     if (++s == S) {
@@ -366,15 +373,17 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
         float* const turn = reinterpret_cast<float*>(ones + ONES_BYTES + NEAR_BYTES) + q * (32 * 17);        // of this warp
         const uint32_t mine = tmem + ((uint32_t)(q * 32) << 16), sums = mine + SUM_COL - NEAR_COLS;     // column c's sum: sums + c
         float* const here = reinterpret_cast<float*>(ones + ONES_BYTES) + row;      // [NEAR_COLS sums, bias gradient][128 rows]
+        // Spans read; negative from the first wait on that ran out: nothing comes behind it, and the barrier's other parity, which the next wait would ask for, has long
+        // passed.  This warp then reads no accumulators and announces none as read (the instructions stop, and with them the other CTA's warps); its results are NaN.
         int done = 0;
         for (int u = pair; u < n_units; u += pairs) {
             const Unit w = unit_of(a, u);
             int m, n;
             tile_at(a, w.tile, &m, &n);
-            bool ok = true;
             for (int k = w.k0; k < w.k1; k += SPAN, ++done) {
                 const bool first = k == w.k0;
-                ok = warp_wait_for(acc_ready, (uint32_t)(done & 1), gave_up) && ok;
+                if (done >= 0 && !warp_wait_for<PROBE>(acc_ready, (uint32_t)(done & 1), gave_up)) done = -1;
+                if (done < 0) break;
                 fence_after_sync();
                 // 16 columns at a time: with 32 registers spill, and 4096 -> 4096 takes 4 % longer
                 for (int g = 0; g < a.nt; g += 16) {
@@ -411,13 +420,13 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
             const int o = m * TILE_M + (int)rank * HALF_M + row, i0 = n * a.nt;
             float* part = w.cut ? a.part + (((size_t)w.part * a.rest + (w.tile - a.whole)) * 2 + rank) * part_floats(a.nt) : nullptr;
             for (int g = 0; g < a.nt; g += 16) {
-                float r[16], v[16];                      // v: channels in order, see codes2; where a wait was given up the results are NaN
+                float r[16], v[16];                      // v: channels in order, see codes2
                 if (g < NEAR_COLS) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) r[e] = here[(g + e) * HALF_M];
                 } else tmem_ld16(sums + g, r);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = ok ? r[(e & 3) == 1 ? e + 1 : (e & 3) == 2 ? e - 1 : e] : __uint_as_float(0x7fc00000u);
+                for (int e = 0; e < 16; ++e) v[e] = done >= 0 ? r[(e & 3) == 1 ? e + 1 : (e & 3) == 2 ? e - 1 : e] : __uint_as_float(0x7fc00000u);
                 if (w.cut) {
                     // four columns of 32 rows side by side
 #pragma unroll
@@ -454,7 +463,7 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
                 }
             }
             if (a.db && n == 0) {
-                const float b = ok ? here[NEAR_COLS * HALF_M] : __uint_as_float(0x7fc00000u);
+                const float b = done >= 0 ? here[NEAR_COLS * HALF_M] : __uint_as_float(0x7fc00000u);
                 if (w.cut) part[(size_t)HALF_M * a.nt + row] = b;
                 else if (o < a.co) a.db[o] = a.add ? a.db[o] + b : b;
             }
@@ -530,7 +539,7 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 if (i0 + j * SETS >= total || !ok) continue;
-                if (!(ok = warp_wait_for(empty(s), parity, gave_up))) continue;
+                if (!(ok = warp_wait_for<PROBE>(empty(s), parity, gave_up))) continue;
                 if (have) {
                     uint8_t* b = b0 + s * STAGE;
 #pragma unroll
@@ -589,7 +598,7 @@ template <int MODE> __global__ void __launch_bounds__(Form<MODE>::THREADS, 1) wg
                         }
                     }
                 }
-                if (!(ok = warp_wait_for(empty(s), (uint32_t)((it / S + 1) & 1), gave_up))) break;
+                if (!(ok = warp_wait_for<PROBE>(empty(s), (uint32_t)((it / S + 1) & 1), gave_up))) break;
                 uint8_t* const d = base + s * STAGE + at;
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
@@ -689,9 +698,9 @@ struct Plan {
     size_t scratch() const { return parts > 1 ? (size_t)parts * rest * 2 * part_floats(nt) : 0; }
 };
 
-template <int MODE> void launch(const CUtensorMap& dy, const WArgs& a, int pairs, cudaStream_t st) {
-    smem_limit_once<150 + MODE>(wgrad_kernel<MODE>, Form<MODE>::SMEM);
-    launch_pdl_cluster(wgrad_kernel<MODE>, 2 * pairs, Form<MODE>::THREADS, 2, Form<MODE>::SMEM, st, dy, a);
+template <int MODE, bool PROBE = false> void launch(const CUtensorMap& dy, const WArgs& a, int pairs, cudaStream_t st) {
+    smem_limit_once<150 + 2 * MODE + PROBE>(wgrad_kernel<MODE, PROBE>, Form<MODE>::SMEM);
+    launch_pdl_cluster(wgrad_kernel<MODE, PROBE>, 2 * pairs, Form<MODE>::THREADS, 2, Form<MODE>::SMEM, st, dy, a);
 }
 
 }  // namespace
@@ -699,7 +708,7 @@ template <int MODE> void launch(const CUtensorMap& dy, const WArgs& a, int pairs
 size_t ckpt8_wgrad_scratch(int dtype, size_t rows, int ci, int co) { return rows ? Plan(rows, ci, co, dtype).scratch() : 0; }
 
 void ckpt8_wgrad(int dtype, const void* codes, const void* exps, const void* dy, size_t lddy, size_t rows, int ci, int co, float* dw, float* db, bool accumulate,
-                 float* scratch, int* err, cudaStream_t st) {
+                 float* scratch, int* err, cudaStream_t st, int silent_after) {
     if (!rows) {
         if (accumulate) return;
         cudaMemsetAsync(dw, 0, (size_t)ci * co * 4, st);
@@ -712,6 +721,8 @@ void ckpt8_wgrad(int dtype, const void* codes, const void* exps, const void* dy,
     a.dy = dy; a.lddy = lddy; a.groups = ((size_t)ci + GROUP - 1) / GROUP; a.pitch = a.groups * GROUP;
     a.rows = (unsigned)rows; a.ci = ci; a.co = co; a.nt = p.nt; a.tm = p.tm; a.tn = p.tn; a.steps = p.steps;
     a.whole = p.whole; a.rest = p.rest; a.parts = p.parts; a.dw = dw; a.db = db; a.part = scratch; a.add = accumulate ? 1 : 0; a.err = err;
+    a.silent_after = silent_after;
+    const bool probe = silent_after >= 0;
     const bool f32 = dtype == AST_F32;
     const bool pairs = reinterpret_cast<uintptr_t>(dy) % 8 == 0 && lddy % 2 == 0 && co % 2 == 0;
     alignas(64) CUtensorMap map{};
@@ -725,8 +736,8 @@ void ckpt8_wgrad(int dtype, const void* codes, const void* exps, const void* dy,
         const double n_w = (double)ci * co;
         LaunchScope ls(K_CKPT8_WGRAD, rows * (a.pitch + a.groups + co * (f32 ? 4.0 : 2.0)) + 4.0 * (n_w + co), 2.0 * rows * n_w, st);
         switch (mode) {
-            case DY_COPY: launch<DY_COPY>(map, a, p.pairs, st); break;
-            case DY_F32: launch<DY_F32>(map, a, p.pairs, st); break;
+            case DY_COPY: probe ? launch<DY_COPY, true>(map, a, p.pairs, st) : launch<DY_COPY>(map, a, p.pairs, st); break;
+            case DY_F32: probe ? launch<DY_F32, true>(map, a, p.pairs, st) : launch<DY_F32>(map, a, p.pairs, st); break;
             case DY_F32_ANY: launch<DY_F32_ANY>(map, a, p.pairs, st); break;
             default: launch<DY_BF16_ANY>(map, a, p.pairs, st);
         }

@@ -333,9 +333,10 @@ void ckpt8_backward(int dtype, int act, const void* codes, const void* exps, con
 // floats of scratch that ckpt8_wgrad needs
 size_t ckpt8_wgrad_scratch(int dtype, size_t rows, int ci, int co);
 // dw[co][ci] (+)= sum over rows of dy * x as kept, db[co] (may be null) (+)= sum of dy.
-// err (may be null): set to 1 if a bounded wait ran out; the sums are NaN then
+// err (may be null): set to 1 if a bounded wait ran out; the sums of the tiles it concerns are NaN then.  silent_after >= 0: the self-test's kernels, whose first
+// pair of CTAs stops after that many steps (dy that lies as tensor copies or pairs of float32 numbers need it)
 void ckpt8_wgrad(int dtype, const void* codes, const void* exps, const void* dy, size_t lddy, size_t rows, int ci, int co, float* dw, float* db, bool accumulate,
-                 float* scratch, int* err, cudaStream_t st);
+                 float* scratch, int* err, cudaStream_t st, int silent_after = -1);
 
 // one warp waits `limit` polls on an mbarrier nobody arrives at; sets *err = 1 when the wait gave up
 void launch_bounded_wait_probe(int* err, unsigned limit, cudaStream_t st);

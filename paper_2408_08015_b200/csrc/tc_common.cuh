@@ -148,8 +148,8 @@ __device__ __forceinline__ bool named_bar_and(uint32_t id, uint32_t threads, boo
 __device__ __forceinline__ void named_bar_sync(uint32_t id, uint32_t threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // Bounded wait that also gives up as soon as another role has raised the abort flag.
-__device__ __forceinline__ bool mbar_wait_abortable(uint32_t mbar, uint32_t parity, volatile int* abort_flag) {
-    for (uint32_t i = 0; i < WAIT_LIMIT; ++i) {
+__device__ __forceinline__ bool mbar_wait_abortable(uint32_t mbar, uint32_t parity, volatile int* abort_flag, uint32_t limit = WAIT_LIMIT) {
+    for (uint32_t i = 0; i < limit; ++i) {
         if (mbar_try_wait(mbar, parity)) return true;
         if (*abort_flag) return false;
         if (i > 32) __nanosleep(32);
