@@ -284,8 +284,9 @@ template <int MODE, bool PROBE> __global__ void __launch_bounds__(Form<MODE>::TH
                 const Unit w = unit_of(a, u);
                 int m, n;
                 tile_at(a, w.tile, &m, &n);
-                const int x = m * TILE_M + (int)rank * HALF_M, y1 = w.k1 * ROWS;
-                for (int y = w.k0 * ROWS; y < y1; y += ROWS) {
+                const int x = m * TILE_M + (int)rank * HALF_M;
+                for (int k = w.k0; k < w.k1; ++k) {
+                    const int y = k * ROWS;              // below 2^31; the row behind the last step's need not be
                     if (!(ok = wait_for<PROBE>(empty(s), parity, gave_up))) break;
                     const uint32_t dst = smem_u32(base) + s * STAGE;
                     if (rank == 0) mbar_expect_tx(full(s), 2 * A_BYTES);
