@@ -268,7 +268,7 @@ int asteroid_embedding_forward(const void* table, int table_dtype, const int32_t
  * written, zeros for tokens that do not occur (the first micro-batch of a round); else the sums are added to grad and the rows of
  * tokens that do not occur are left alone (the further micro-batches); in these additions numbers below 2^-126 may count as zero.  The tokens are sorted by id and every run of equal ids is summed in a fixed order:
  * the same inputs give the same bits.  workspace: 16-byte aligned DEVICE memory of at least asteroid_embedding_workspace bytes, not
- * shared by calls that may overlap. */
+ * shared by calls that may overlap; one for some rows suffices for fewer. */
 size_t asteroid_embedding_workspace(size_t rows, int dim);
 int asteroid_embedding_backward(const int32_t* ids, const void* dy, size_t lddy, size_t rows, int vocab, int dim, float scale, int dtype, float* grad,
                                 int accumulate, void* workspace, size_t workspace_bytes, void* stream);

@@ -593,11 +593,21 @@ int bits_of(unsigned v) {
 
 // Sorted tokens of a warp: as many as leave some 4 warps for each of the 4 schedulers of 148 multiprocessors, at most 32.  Fewer make more open ends, more make
 // longer chains of requests.
+constexpr size_t FEW_WARPS = 2368;
 int per_warp_of(size_t rows, int dim) {
     const size_t slabs = ((size_t)dim + COLS - 1) / COLS;
     int r = 32;
-    while (r > 4 && (rows + r - 1) / r * slabs < 2368) r >>= 1;
+    while (r > 4 && (rows + r - 1) / r * slabs < FEW_WARPS) r >>= 1;
     return r;
+}
+size_t run_blocks(size_t rows, int per_warp) { return (rows + RUN_WARPS * per_warp - 1) / (RUN_WARPS * per_warp); }
+// The most blocks that `rows` rows or fewer take.  From some row count on warps have twice as many tokens and there are half as many blocks: those of
+// each length are largest at the last row count that has it.
+size_t most_blocks(size_t rows, int dim) {
+    const size_t slabs = ((size_t)dim + COLS - 1) / COLS;
+    size_t most = run_blocks(rows, per_warp_of(rows, dim));
+    for (int r = 4; r < 32; r <<= 1) most = std::max(most, run_blocks(std::min(rows, 2 * r * ((FEW_WARPS - 1) / slabs)), r));
+    return most;
 }
 
 constexpr size_t MAX_ROWS = ((size_t)1 << 31) - 1, MAX_ELEMS = (size_t)1 << 40;
@@ -619,7 +629,7 @@ int launched() {
 }
 
 // What a gradient of so many tokens needs: at most `part` tokens are sorted at a time, by pairs (two lists where they are merged), then the partial
-// rows of the blocks' ends.
+// rows of the blocks' ends.  `bytes` suffices for every smaller number of tokens as well.
 struct BackwardPlan {
     size_t part, pair_bytes, bytes;
     int per_warp;
@@ -627,9 +637,8 @@ struct BackwardPlan {
         part = std::min(rows, (size_t)MAX_CHUNKS * CHUNK);
         part += part & 1;                                  // the second list and the partial rows start at 16 bytes
         per_warp = per_warp_of(part, dim);
-        const size_t blocks = (part + RUN_WARPS * per_warp - 1) / (RUN_WARPS * per_warp);
         pair_bytes = part * sizeof(Pair) * (part > CHUNK ? 2 : 1);
-        bytes = rows ? pair_bytes + blocks * 2 * dim * sizeof(float) : 0;
+        bytes = rows ? pair_bytes + most_blocks(part, dim) * 2 * dim * sizeof(float) : 0;
     }
 };
 
@@ -721,7 +730,7 @@ int asteroid_embedding_backward(const int32_t* ids, const void* dy, size_t lddy,
         RunArgs a{};
         a.s = sorted; a.dy = dy; a.lddy = lddy; a.grad = grad; a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.pair_bytes);
         a.n = n; a.vocab = (unsigned)vocab; a.dim = dim; a.per_warp = plan.per_warp; a.scale = scale; a.add = add;
-        const unsigned blocks = (n + RUN_WARPS * a.per_warp - 1) / (RUN_WARPS * a.per_warp), slabs = (unsigned)((dim + COLS - 1) / COLS);
+        const unsigned blocks = (unsigned)run_blocks(n, a.per_warp), slabs = (unsigned)((dim + COLS - 1) / COLS);
         const int N = dtype == AST_F32 ? 4 : 8;
         const bool vec = dim % N == 0 && lddy % N == 0 && (reinterpret_cast<uintptr_t>(dy) | reinterpret_cast<uintptr_t>(grad)) % 16 == 0;
         {
