@@ -251,7 +251,7 @@ int asteroid_ckpt8_act_backward(int act, const void* ckpt, const void* dy, size_
  * the device only: the same inputs give the same bits.  Should a wait inside the kernel run out, the tiles of dw, with their entries of db,
  * that it concerns are NaN, all of them.  workspace: 16-byte aligned DEVICE memory of at least
  * asteroid_ckpt8_linear_wgrad_workspace bytes as asked for on this device (may be 0, then workspace may be NULL), not shared by calls that may
- * overlap.
+ * overlap; one for some rows suffices for fewer.
  * c_in, c_out <= 65536. */
 size_t asteroid_ckpt8_linear_wgrad_workspace(size_t rows, int c_in, int c_out, int dtype);
 int asteroid_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db,

@@ -440,7 +440,7 @@ static int bad_widths(size_t rows, int c_in, int c_out, int dtype) {
 
 size_t asteroid_ckpt8_linear_wgrad_workspace(size_t rows, int c_in, int c_out, int dtype) {
     if (bad_widths(rows, c_in, c_out, dtype)) return 0;
-    return ckpt8_wgrad_scratch(dtype, rows, c_in, c_out) * sizeof(float);
+    return ckpt8_wgrad_most_scratch(dtype, rows, c_in, c_out) * sizeof(float);
 }
 
 // checks and launches of both calls
@@ -450,7 +450,7 @@ static int linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t ro
     if (rc || (rc = bad_matrix("lddy out of range", dy, lddy, rows, c_out, dtype)) || (rc = bad_ckpt(ckpt, rows))) return rc;
     if (!dw) return report_error(AST_ERR_ARG, "null argument");
     if ((reinterpret_cast<uintptr_t>(dw) | reinterpret_cast<uintptr_t>(db)) % 4) return report_error(AST_ERR_ARG, "a tensor does not start at an element of its type");
-    const size_t need = ckpt8_wgrad_scratch(dtype, rows, c_in, c_out) * sizeof(float);
+    const size_t need = ckpt8_wgrad_most_scratch(dtype, rows, c_in, c_out) * sizeof(float);
     if (need && (!workspace || workspace_bytes < need)) return report_error(AST_ERR_ARG, "the workspace is too small");
     if (need && reinterpret_cast<uintptr_t>(workspace) % 16) return report_error(AST_ERR_ARG, "a workspace must start at a 16-byte boundary");
     ckpt8_wgrad(dtype, ckpt, exps_of(ckpt, rows, c_in), dy, lddy, rows, c_in, c_out, dw, db, accumulate != 0, static_cast<float*>(workspace), err, st, silent_after);

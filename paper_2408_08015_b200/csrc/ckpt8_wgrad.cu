@@ -674,21 +674,22 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const WArgs a) {
 // How the tiles are dealt out.  A step of 64 rows takes a pair 0.45 us (float32 1.5), starting a unit and storing its accumulators some 5 us; parts are written and read
 // again at 6 bytes a picosecond by a kernel of 3 us.
 struct Plan {
-    int nt, tm, tn, steps, pairs, whole, rest, parts;
+    int nt, tm, tn, steps, pairs, whole, rest, parts, all;
+    double step_us;
     Plan(size_t rows, int ci, int co, int dtype) {
         nt = ci > 128 ? 256 : 128;
         tm = (co + TILE_M - 1) / TILE_M;
         tn = (ci + nt - 1) / nt;
         steps = (int)((rows + ROWS - 1) / ROWS);
-        const int all = sm_count() / 2, tiles = tm * tn;
+        all = sm_count() / 2;
+        const int tiles = tm * tn;
         whole = tiles / all * all;
         rest = tiles - whole;
         parts = 1;
-        const double step_us = (dtype == AST_F32 ? 1.5 : 0.45) * nt / 256;
+        step_us = (dtype == AST_F32 ? 1.5 : 0.45) * nt / 256;
         double best = 1e300;
-        for (int s = 1; rest && s <= 64 && s <= std::max(1, steps / 2); ++s) {
-            const int rounds = (rest * s + all - 1) / all;
-            const double us = rounds * ((steps + s - 1) / s * step_us + 5.0) + (s > 1 ? 3.0 + 8e-6 * s * rest * TILE_M * nt / 6.0 : 0.0);
+        for (int s = 1; rest && s <= MAX_PARTS && s <= std::max(1, steps / 2); ++s) {
+            const double us = rounds(s) * ((steps + s - 1) / s * step_us + UNIT_US) + join_us(s);
             if (us < best) {
                 best = us;
                 parts = s;
@@ -696,7 +697,28 @@ struct Plan {
         }
         pairs = std::min(all, whole ? all : rest * parts);
     }
-    size_t scratch() const { return parts > 1 ? (size_t)parts * rest * 2 * part_floats(nt) : 0; }
+    static constexpr int MAX_PARTS = 64;
+    static constexpr double UNIT_US = 5.0;
+    int rounds(int s) const { return (rest * s + all - 1) / all; }
+    double join_us(int s) const { return s > 1 ? 3.0 + 8e-6 * s * rest * TILE_M * nt / 6.0 : 0.0; }
+    // No smaller number of rows takes more parts.  The number chosen goes up and down with the rows; s parts are chosen only where they cost less than any t < s, which
+    // with the steps of a part rounded down for s and up for t bounds the number of steps on one side for each t.
+    int most_parts() const {
+        for (int s = std::min(MAX_PARTS, steps / 2); rest && s > 1; --s) {
+            double lo = 2.0 * s, hi = steps;
+            for (int t = 1; t < s && lo <= hi; ++t) {
+                const double slope = step_us * ((double)rounds(s) / s - (double)rounds(t) / t);
+                const double more = rounds(t) * (step_us * (t - 1) / t + UNIT_US) + join_us(t) - rounds(s) * UNIT_US - join_us(s) + 1e-6;
+                // steps * slope < more, but for arithmetic errors far below 1e-6 us
+                if (slope > 1e-12) hi = std::min(hi, more / slope);
+                else if (slope < -1e-12) lo = std::max(lo, more / slope);
+                else if (more < 0) hi = 0;
+            }
+            if (lo <= hi) return s;
+        }
+        return 1;
+    }
+    size_t scratch(int p) const { return p > 1 ? (size_t)p * rest * 2 * part_floats(nt) : 0; }
 };
 
 template <int MODE, bool PROBE = false> void launch(const CUtensorMap& dy, const WArgs& a, int pairs, cudaStream_t st) {
@@ -706,7 +728,14 @@ template <int MODE, bool PROBE = false> void launch(const CUtensorMap& dy, const
 
 }  // namespace
 
-size_t ckpt8_wgrad_scratch(int dtype, size_t rows, int ci, int co) { return rows ? Plan(rows, ci, co, dtype).scratch() : 0; }
+size_t ckpt8_wgrad_scratch(int dtype, size_t rows, int ci, int co) {
+    const Plan p(rows, ci, co, dtype);
+    return p.scratch(p.parts);
+}
+size_t ckpt8_wgrad_most_scratch(int dtype, size_t rows, int ci, int co) {
+    const Plan p(rows, ci, co, dtype);
+    return p.scratch(std::max(p.parts, p.most_parts()));
+}
 
 void ckpt8_wgrad(int dtype, const void* codes, const void* exps, const void* dy, size_t lddy, size_t rows, int ci, int co, float* dw, float* db, bool accumulate,
                  float* scratch, int* err, cudaStream_t st, int silent_after) {
@@ -745,7 +774,7 @@ void ckpt8_wgrad(int dtype, const void* codes, const void* exps, const void* dy,
     }
     if (p.parts > 1) {
         const size_t threads = ((size_t)p.nt / 4 * HALF_M + HALF_M) * 2 * p.rest;
-        LaunchScope ls(K_REDUCE_SPLITS, 4.0 * p.scratch() + 4.0 * p.rest * TILE_M * p.nt, 0.0, st);
+        LaunchScope ls(K_REDUCE_SPLITS, 4.0 * p.scratch(p.parts) + 4.0 * p.rest * TILE_M * p.nt, 0.0, st);
         launch_pdl(sum_parts_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, a);
     }
 }

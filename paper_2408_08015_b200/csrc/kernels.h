@@ -330,8 +330,9 @@ void ckpt8_forward(int dtype, int act, const void* x, size_t ldx, size_t rows, i
 // dy null: out = the values kept; else out = dy * act'(the values kept)
 void ckpt8_backward(int dtype, int act, const void* codes, const void* exps, const void* dy, size_t lddy, size_t rows, int cols, void* out, size_t ldo,
                     cudaStream_t st);
-// floats of scratch that ckpt8_wgrad needs
+// floats of scratch that ckpt8_wgrad needs, for so many rows and for any number up to that
 size_t ckpt8_wgrad_scratch(int dtype, size_t rows, int ci, int co);
+size_t ckpt8_wgrad_most_scratch(int dtype, size_t rows, int ci, int co);
 // dw[co][ci] (+)= sum over rows of dy * x as kept, db[co] (may be null) (+)= sum of dy.
 // err (may be null): set to 1 if a bounded wait ran out; the sums of the tiles it concerns are NaN then.  silent_after >= 0: the self-test's kernels, whose first
 // pair of CTAs stops after that many steps (dy that lies as tensor copies or pairs of float32 numbers need it)
