@@ -852,7 +852,7 @@ static int bn_reduce_target(const asteroid_stage* s, int v) {
 static bool wgrad_from_codes(const asteroid_stage* s, const Unit& u) {
     if (!s->ckpt8 || u.kind != U_CONV || u.b_off < 0 || u.l_bn >= 0 || u.act != ACT_NONE) return false;
     const Val& a = s->vals[u.in];
-    return !a.affine && a.act == ACT_NONE && a.c % AST_CKPT8_GROUP == 0 && a.c <= 65536 && u.g.co <= 65536 && ckpt8_wgrad_scratch(s->dtype, s->B, a.c, u.g.co) <= s->scratch_floats;
+    return !a.affine && a.act == ACT_NONE && a.c % AST_CKPT8_GROUP == 0 && a.c <= 65536 && u.g.co <= 65536;
 }
 
 static int backward_impl(asteroid_stage* s, int slot, const void* dy, void* dx, cudaStream_t st) {
@@ -1291,8 +1291,11 @@ static int create_impl(const ast_layer* net, int n_layers, int first, int last, 
     s->scratch_floats = (size_t)8 << 20;
     for (const auto& u : s->units)
         if (u.kind == U_CONV) s->scratch_floats = std::max(s->scratch_floats, (size_t)4 * u.g.co * u.g.k * u.g.k * u.g.ci);
-    if ((rc = arena_alloc(s, "scratch", &s->scratch, s->scratch_floats * 4, &work))) return rc;
-    if ((rc = arena_alloc(s, "scratch of the second stream", &s->scratch_side, s->scratch_floats * 4, &work))) return rc;
+    size_t scratch = s->scratch_floats;            // what weight gradients from checkpoints need beyond it changes no other layer's split
+    for (const auto& u : s->units)
+        if (wgrad_from_codes(s, u)) scratch = std::max(scratch, ckpt8_wgrad_scratch(s->dtype, s->B, s->vals[u.in].c, u.g.co));
+    if ((rc = arena_alloc(s, "scratch", &s->scratch, scratch * 4, &work))) return rc;
+    if ((rc = arena_alloc(s, "scratch of the second stream", &s->scratch_side, scratch * 4, &work))) return rc;
     for (auto& u : s->units)
         if (conv3_s2_tc_supported(s, u)) {
             u.up_off = (long)s->up_bytes;
