@@ -238,7 +238,7 @@ size_t asteroid_ckpt8_bytes(size_t rows, int cols);
 int asteroid_ckpt8_pack(const void* x, size_t ldx, size_t rows, int cols, int dtype, void* ckpt, void* stream);
 int asteroid_ckpt8_unpack(const void* ckpt, size_t rows, int cols, int dtype, void* x, size_t ldx, void* stream);
 /* Activation layer, act = AST_RELU6, AST_RELU, AST_SILU or AST_GELU (x * Phi(x), Phi the normal distribution function; not a layer
- * op of a stage): y = act(x), and x is packed in the same pass.  NaN gives NaN. */
+ * op of a stage): y = act(x), and x is packed in the same pass.  NaN gives NaN.  GELU of bfloat16 values takes exp(-x^2 / 2) below 2^-126 for zero. */
 enum { AST_GELU = 10 };
 int asteroid_ckpt8_act_forward(int act, const void* x, size_t ldx, size_t rows, int cols, int dtype, void* y, size_t ldy, void* ckpt, void* stream);
 /* Its backward from the checkpoint of x: dx = dy * act'(x as kept); 0 where act' is 0 at a kink or in a flat part, whatever dy; NaN where x
