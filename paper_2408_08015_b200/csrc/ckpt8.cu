@@ -2,7 +2,7 @@
 //
 // All passes are elementwise over groups of 32 columns and bound by memory: a thread owns one 16-byte vector of the storage type (4 or 8
 // values), the 8 or 4 lanes of a group find its largest magnitude by shuffles, and every tensor is read and written once.  Instructions are next: a SiLU step
-// of 16 384 x 2048 bfloat16 numbers takes 56 us, 84 % of the memory's rate, with the schedulers busy in three cycles of four; packing and unpacking 100 352 x 256 26 us, of
+// of 16 384 x 2048 bfloat16 numbers takes 56 us, 84 % of the memory's rate, with the schedulers busy in two cycles of three; packing and unpacking 100 352 x 256 26 us, of
 // which memory needs 20.
 #include "../../include/asteroid.h"
 #include "ckpt8.cuh"
@@ -463,9 +463,8 @@ size_t asteroid_ckpt8_linear_wgrad_workspace(size_t rows, int c_in, int c_out, i
     return ckpt8_wgrad_most_scratch(dtype, rows, c_in, c_out) * sizeof(float);
 }
 
-// checks and launches of both calls
-static int linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db, int accumulate,
-                        void* workspace, size_t workspace_bytes, int* err, int silent_after, cudaStream_t st) {
+static int bad_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, const float* dw, const float* db,
+                            const void* workspace, size_t workspace_bytes) {
     int rc = bad_widths(rows, c_in, c_out, dtype);
     if (rc || (rc = bad_matrix("lddy out of range", dy, lddy, rows, c_out, dtype)) || (rc = bad_ckpt(ckpt, rows))) return rc;
     if (!dw) return report_error(AST_ERR_ARG, "null argument");
@@ -473,30 +472,37 @@ static int linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t ro
     const size_t need = ckpt8_wgrad_most_scratch(dtype, rows, c_in, c_out) * sizeof(float);
     if (need && (!workspace || workspace_bytes < need)) return report_error(AST_ERR_ARG, "the workspace is too small");
     if (need && reinterpret_cast<uintptr_t>(workspace) % 16) return report_error(AST_ERR_ARG, "a workspace must start at a 16-byte boundary");
-    ckpt8_wgrad(dtype, ckpt, exps_of(ckpt, rows, c_in), dy, lddy, rows, c_in, c_out, dw, db, accumulate != 0, static_cast<float*>(workspace), err, st, silent_after);
-    return launched();
+    return AST_OK;
 }
 
 int asteroid_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db,
                                 int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
-    return linear_wgrad(ckpt, dy, lddy, rows, c_in, c_out, dtype, dw, db, accumulate, workspace, workspace_bytes, nullptr, -1, (cudaStream_t)stream);
+    if (int rc = bad_linear_wgrad(ckpt, dy, lddy, rows, c_in, c_out, dtype, dw, db, workspace, workspace_bytes)) return rc;
+    ckpt8_wgrad(dtype, ckpt, exps_of(ckpt, rows, c_in), dy, lddy, rows, c_in, c_out, dw, db, accumulate != 0, static_cast<float*>(workspace), nullptr,
+                (cudaStream_t)stream);
+    return launched();
 }
 
 int asteroid_selftest_ckpt8_linear_wgrad(const void* ckpt, const void* dy, size_t lddy, size_t rows, int c_in, int c_out, int dtype, float* dw, float* db,
                                          int accumulate, void* workspace, size_t workspace_bytes, int silent_after) {
+    if (int rc = bad_linear_wgrad(ckpt, dy, lddy, rows, c_in, c_out, dtype, dw, db, workspace, workspace_bytes)) return rc;
     const size_t unit = dtype == AST_F32 ? 2 : 8;
     if (silent_after < 0 || rows < 1 || lddy % unit || reinterpret_cast<uintptr_t>(dy) % (unit == 2 ? 8 : 16) || (dtype == AST_F32 && c_out % 2))
         return report_error(AST_ERR_ARG, "the self-test takes rows of dy at 16-byte (float32: 8-byte) boundaries, and a number of steps");
     int *err = nullptr, h = 0;
     cudaError_t e = cudaMalloc((void**)&err, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(err, 0, sizeof(int));
-    int rc = AST_OK;
-    if (e == cudaSuccess) rc = linear_wgrad(ckpt, dy, lddy, rows, c_in, c_out, dtype, dw, db, accumulate, workspace, workspace_bytes, err, silent_after, 0);
-    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) {
+        ckpt8_wgrad(dtype, ckpt, exps_of(ckpt, rows, c_in), dy, lddy, rows, c_in, c_out, dw, db, accumulate != 0, static_cast<float*>(workspace), err, 0, silent_after);
+        e = cudaDeviceSynchronize();
+    }
     if (e == cudaSuccess) e = cudaMemcpy(&h, err, sizeof h, cudaMemcpyDeviceToHost);
     cudaFree(err);
-    if (rc) return rc;
-    if (e != cudaSuccess) return report_error(AST_ERR_CUDA, cudaGetErrorString(e));
+    if (e == cudaSuccess) e = cudaGetLastError();
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return report_error(AST_ERR_CUDA, cudaGetErrorString(e));
+    }
     return h ? report_error(AST_ERR_TIMEOUT, "a bounded device-side wait expired (self-test: expected)") : AST_OK;
 }
 
