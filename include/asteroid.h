@@ -247,7 +247,7 @@ int asteroid_ckpt8_act_backward(int act, const void* ckpt, const void* dy, size_
                                 void* stream);
 /* Parameter gradients of a linear layer from the checkpoint of its input x [rows][c_in] and the gradient dy [rows][c_out] of its output:
  * dw[o][i] = sum over rows of dy[r][o] * (x as kept)[r][i], db[o] = sum over rows of dy[r][o] (db may be NULL), float32 sums, added to
- * what dw and db hold if `accumulate`, else written.  rows = 0 gives zeros.  The order of the sums depends on the sizes, the type and
+ * what dw and db hold if `accumulate`, else written; bits of a float32 dy below 2^-133 count as zero.  rows = 0 gives zeros.  The order of the sums depends on the sizes, the type and
  * the device only: the same inputs give the same bits.  Should a wait inside the kernel run out, the tiles of dw, with their entries of db,
  * that it concerns are NaN, all of them.  workspace: 16-byte aligned DEVICE memory of at least
  * asteroid_ckpt8_linear_wgrad_workspace bytes as asked for on this device (may be 0, then workspace may be NULL), not shared by calls that may

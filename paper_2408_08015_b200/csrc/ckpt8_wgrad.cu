@@ -3,11 +3,11 @@
 //
 // One product on the tensor cores with the rows as the reduction, both operands MN-major as they lie in memory.  A kept value is a bfloat16 number,
 // so the codes become the exact operand in registers on their way to shared memory and never exist in 16 bits in global memory.  float32 gradients
-// are cut into three bfloat16 terms of 8 bits each, exact too, and three instructions take the place of one.
+// are cut into three bfloat16 terms of 8 bits each, exact too but for bits below 2^-133, and three instructions take the place of one.
 //
 // What bounds it is shared memory, where the warps write the operand that the tensor core reads next to the other, and the issue of the warps that convert
 // and of the one that feeds the tensor core: a step of 64 rows takes 750 to 800 cycles, 605 with the conversion left out, the instructions 512.  4096 -> 4096 over 32 768
-// rows: 1.07 to 1.1 ms, 1.0 PFLOP/s, at the 1.15 to 1.2 GHz that the power cap leaves; 512 -> 2048 over 16 384 rows: 50 us, 28 of them steps.  A pair of CTAs
+// rows: 1.09 to 1.12 ms from one B200 to another, 0.98 to 1.01 PFLOP/s, at the 1.15 to 1.2 GHz that the power cap leaves; 512 -> 2048 over 16 384 rows: 50 to 52 us, 28 of them steps.  A pair of CTAs
 // therefore shares one tile of 256 output by up to 256 input channels (tcgen05, cta_group::2): each holds 128 output channels of dy and half of the
 // input channels, and converts half of the codes.  A step is 64 rows.
 //   warp 0        tiled tensor copies of dy (the leading CTA's barrier counts the bytes of both)
@@ -47,9 +47,10 @@ constexpr int NEAR_BYTES = (NEAR_COLS + 1) * HALF_M * 4, TURN_BYTES = 4 * 32 * 1
 enum { DY_COPY = 0, DY_F32 = 1, DY_F32_ANY = 2, DY_BF16_ANY = 3 };  // how dy is read
 template <int MODE> struct Form {
     static constexpr int TERMS = MODE == DY_F32 || MODE == DY_F32_ANY ? 3 : 1;
-    // The tensor core cuts a sum to 24 bits at every addition instead of rounding it, so that sums shrink by up to 2^-24 of themselves with each of the four
+    // The tensor core cuts a sum to 24 bits at every addition instead of rounding it, so that sums shrink by some 2^-24 of themselves with each of the four
     // instructions of a step: over 32768 rows the gradient was off by 2.8e-5 of its norm, over 4096 by 2.4e-6.  After SPAN steps the accumulators are therefore added
-    // to sums of float32, rounded: below 1e-6 whatever the rows.
+    // to sums of float32, rounded.  Normal values on both sides: 8e-7 over 32768 rows.  The worst case, sums of one sign: the at most 112 additions of a span cut up to
+    // 2^-23 each, 1.4e-5, and the sums of the spans round, 2^-24 for each span: 6.3e-6 at 40 000 rows of float32 dy, growing with the rows.
     static constexpr int SPAN = TERMS == 3 ? 6 : 28;
     static constexpr int SETS = MODE == DY_COPY ? 2 : 1;                 // of warps that convert codes
     static constexpr int AHEAD = MODE == DY_COPY ? 1 : 2;                // of its steps whose codes a set requests ahead (three: 4 % slower at 4096 -> 4096)
@@ -671,8 +672,8 @@ __global__ void __launch_bounds__(256) sum_parts_kernel(const WArgs a) {
         for (int h = 0; h < left; ++h) d[h] = s[h];
 }
 
-// How the tiles are dealt out.  A step of 64 rows takes a pair 0.45 us (float32 1.5), starting a unit and storing its accumulators some 5 us; parts are written and read
-// again at 6 bytes a picosecond by a kernel of 3 us.
+// How the tiles are dealt out.  A step of 64 rows takes a pair 0.45 us (float32 1.5; bfloat16 dy through registers some 0.9, which the plan does not tell apart), starting a unit and
+// storing its accumulators some 5 us; parts are written and read again at 6 bytes a picosecond by a kernel of 3 us.
 struct Plan {
     int nt, tm, tn, steps, pairs, whole, rest, parts, all;
     double step_us;
