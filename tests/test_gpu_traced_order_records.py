@@ -45,7 +45,8 @@ def test_order_of_a_traced_backward_in_a_process_of_its_own():
 
 def test_a_session_takes_the_profiles_first():
     def collected():
-        r = subprocess.run([sys.executable, "-m", "pytest", "--collect-only", "-q", "-m", "gpu", "tests"], capture_output=True, text=True, timeout=300, cwd=ROOT)
+        r = subprocess.run([sys.executable, "-m", "pytest", "--collect-only", "-q", "-m", "gpu", "tests"], capture_output=True, text=True, timeout=300, cwd=ROOT,
+                           env={k: v for k, v in os.environ.items() if k != "PYTEST_ADDOPTS"})
         assert r.returncode == 0, r.stdout[-2000:]
         return [l for l in r.stdout.splitlines() if "::" in l]
     ids = collected()
